@@ -498,11 +498,12 @@ __global__ __launch_bounds__(256, 1) void big_kernel(TileArgs p, int32_t splits)
     auto store_tile = [&](const Piece& x) {
         const int64_t m0 = x.tm * int64_t(256), n0 = x.tn * int64_t(256);
         const int64_t left_m = min(int64_t(256), p.a.rows - m0);
-        const int32_t left_n =
-            static_cast<int32_t>(min(int64_t(256), (sizeof(Out) == 2 ? p.b.rows : p.ld) - n0)) - wn * 128;
+        // what a row holds beyond N is the caller's, or, where the sum is in pieces, the workspace's own padding
+        const int64_t left = min(int64_t(256), (splits > 1 ? p.ld : p.b.rows) - n0);
+        const int32_t left_n = static_cast<int32_t>(left) - wn * 128;
         const auto rows = __builtin_amdgcn_make_buffer_rsrc(
             static_cast<uint8_t*>(p.out) + ((x.split * int64_t(p.a.rows) + m0) * p.ld + n0) * kSize, 0,
-            static_cast<uint32_t>(left_m * p.ld * kSize), 0x00027000);
+            static_cast<uint32_t>(((left_m - 1) * p.ld + left) * kSize), 0x00027000);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
