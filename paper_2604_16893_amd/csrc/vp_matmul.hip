@@ -588,6 +588,9 @@ __global__ __launch_bounds__(256, 1) void big_kernel(TileArgs p, int32_t splits)
         const Piece next = locate(now.item + gridDim.x);
         const i32x4 next_a = rows_of(p.a, next.tm, next), next_b = rows_of(p.b, next.tn, next);
         const i32x4 next_sa = scales_of(p.a, next.tm, next), next_sb = scales_of(p.b, next.tn, next);
+        // Where nothing follows, both of the last two fetches are of block 0 of empty buffers: their size less an
+        // offset, which is what a load's address is held against, stays 0.
+        const int32_t second = next.item < items ? 1 : 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -603,7 +606,7 @@ __global__ __launch_bounds__(256, 1) void big_kernel(TileArgs p, int32_t splits)
             bool any = false;
             auto move_on = [&](int part) {   // the next fetches' place
                 if (part == 0) {
-                    at = over ? next.first : at + 1;
+                    at = over ? next.first : at + (left == 1 ? second : 1);
                     any = over || (at & 3) == 0;
                     word += any;
                 }

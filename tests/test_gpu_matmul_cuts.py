@@ -42,3 +42,12 @@ def test_widest_tiles_leave_the_neighbouring_columns(m, n, k, pad, at, out):
     if (pad, at) == (5, 3):
         check_product(y[:200], vp.Fp8(a.q[:200], a.scale[:200], k, 1), b, k)
         check_product(y[-200:], vp.Fp8(a.q[-200:], a.scale[-200:], k, 1), b, k)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(130, 38488, 500), (38488, 130, 500), (255, 38400, 2000)])
+def test_widest_tiles_of_fewer_rows_than_a_tile(m, n, k, out):
+    """One operand has fewer rows than a tile, so that no load past its end lands in the matrix itself."""
+    a = vp.fp8_quantize(rand((m, k), 1, spread=0.7))
+    b = vp.fp8_quantize(rand((n, k), 2, spread=0.7), 128)
+    check_product(vp.fp8_matmul(a, b, out), a, b, k)
