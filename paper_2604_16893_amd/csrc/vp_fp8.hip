@@ -76,6 +76,29 @@ __device__ __forceinline__ void load_source(const Source& s, const T*, int64_t r
                                             int64_t left, float (&v)[8]) {
     load8<FAR>(static_cast<const T*>(s.x) + r * s.ld + c, left, v);
 }
+// Values in 8 bits reach 448 * 2^127, past f32's 2^128, so a tile whose rows have
+// scales of their own holds them kDown powers of two smaller, which is exact: they
+// are multiples of 2^-135, and f32's least is 2^-149.
+constexpr int kDown = 8;
+__device__ __forceinline__ float held_scale(uint32_t byte) {
+    return byte == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(1.0f, static_cast<int>(byte) - 127 - kDown);
+}
+// scale_byte of a largest magnitude held so: m * 2^e with m in [0.5, 1), below f32's normal numbers too.
+__device__ __forceinline__ uint32_t held_scale_byte(uint32_t top) {
+    if (top >= 0x7f800000u) return 255u;
+    const float v = __uint_as_float(top);
+    const int b = __builtin_amdgcn_frexp_expf(v) + kDown + 118 + (__builtin_amdgcn_frexp_mantf(v) > 0.875f ? 1 : 0);
+    return static_cast<uint32_t>(top == 0 ? 1 : max(b, 1));
+}
+// The factor from a value held so to its quotient by a byte's power of two, 2^(127 + kDown - byte), as far as f32 holds
+// it; the rest of it, for the least bytes.
+__device__ __forceinline__ float held_inverse_scale(uint32_t byte) {
+    return byte == 255u ? __uint_as_float(0x7fc00000u) : ldexpf(1.0f, min(127 + kDown - static_cast<int>(byte), 127));
+}
+__device__ __forceinline__ float held_inverse_rest(uint32_t byte) {
+    return ldexpf(1.0f, max(kDown - static_cast<int>(byte), 0));
+}
+
 template <bool FAR>
 __device__ __forceinline__ void load_source(const Source& s, const uint8_t*, int64_t r, int32_t c,
                                             int64_t left, float (&v)[8]) {
@@ -86,7 +109,7 @@ __device__ __forceinline__ void load_source(const Source& s, const uint8_t*, int
     }
     const u32x2 q = *reinterpret_cast<const u32x2*>(s.in.q + r * s.in.ld + c);   // rows are whole 128s
     // a tile with one scale keeps it: its bytes move as they are
-    unpack8(q, s.in.block == 1 ? scale_value(s.in.scale[r * s.in.sld + c / kBlock]) : 1.0f, v);
+    unpack8(q, s.in.block == 1 ? held_scale(s.in.scale[r * s.in.sld + c / kBlock]) : 1.0f, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : 0.0f;
 }
@@ -112,6 +135,7 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(Source src, int32_t 
     __shared__ __align__(16) uint8_t tile[128 * 128];
     __shared__ uint32_t top[8][128];
     __shared__ __align__(16) float inverse[128];
+    __shared__ float rest[kHeld ? 128 : 1];
     const int t = threadIdx.x, cg = t & 15, rg = t >> 4, wave = t >> 6;
     const int64_t rb = blockIdx.x / static_cast<uint32_t>(tiles_c);
     const int32_t cb = static_cast<int32_t>(blockIdx.x - rb * tiles_c);
@@ -172,14 +196,26 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(Source src, int32_t 
             uint32_t m = 0;
 #pragma unroll
             for (int w = 0; w < 8; ++w) m = max(m, top[w][t]);
-            const uint32_t byte = scale_byte(m);
-            inverse[t] = inverse_scale(byte);
+            const uint32_t byte = kHeld ? held_scale_byte(m) : scale_byte(m);
+            inverse[t] = kHeld ? held_inverse_scale(byte) : inverse_scale(byte);
+            if constexpr (kHeld) rest[t] = held_inverse_rest(byte);
             if (cb * int64_t(128) + t < cols) put_scale(by_cols, cb * int64_t(128) + t, rb, tiles_r, byte);
         }
         __syncthreads();
     }
     const f32x4 low = *reinterpret_cast<const f32x4*>(inverse + cg * 8);
     const f32x4 high = *reinterpret_cast<const f32x4*>(inverse + cg * 8 + 4);
+    if (kHeld && block == 1) {
+        float most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = fmaxf(most, fmaxf(low[j], high[j]));
+        if (most == 0x1p127f) {   // bytes of kDown and less
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i][j] *= rest[cg * 8 + j];
+        }
+    }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float inv = block != 1 ? tile_inverse : j < 4 ? low[j] : high[j - 4];
