@@ -462,7 +462,10 @@ typedef struct vp_fp8 {
     int32_t reserved; /* 0                                                           */
 } vp_fp8;
 
-/* The largest rows or cols of a matrix of the operators below. */
+/* The largest rows or cols of a matrix of the operators below.  (vp_fp8_quantize
+ * with by_cols or block 128 and vp_fp8_transpose: at most 2^32 - 1 tiles of 128 x
+ * 128.  vp_fp8_matmul: at most 2^24 - 1 tiles of 128 x 128 of the result, of 64 x
+ * 64 where K is above 2^25 - 128.  More are VP_ERR_DIMS.) */
 #define VP_MAX_DIM 0x7fffff00
 /* The largest K of vp_fp8_matmul. */
 #define VP_MAX_SUM 0x3ffff80

@@ -74,6 +74,7 @@ struct MatmulArgs {
     bool bf16;
     float* partial;
 };
+// Bytes; -1 where the result has more tiles than a launch takes.
 int64_t matmul_workspace(int64_t m, int64_t n, int64_t k, bool bf16);
 int launch_matmul(const MatmulArgs& a, hipStream_t stream);
 

@@ -20,10 +20,10 @@ constexpr int kItems = 4;
 
 template <class T, bool FAR>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* x, int64_t ld, int32_t cols,
-                                                            int32_t blocks, int64_t total,
+                                                            int32_t blocks, int64_t total, int64_t first_wg,
                                                             Fp8View out) {
     const int lane = threadIdx.x & 15;
-    const int64_t first = blockIdx.x * int64_t(16 * kItems) + (threadIdx.x >> 4);
+    const int64_t first = (first_wg + blockIdx.x) * (16 * kItems) + (threadIdx.x >> 4);
     int64_t row = first / blocks;
     int32_t kb = static_cast<int32_t>(first - row * blocks);
     float v[kItems][8];
@@ -129,16 +129,17 @@ __device__ __forceinline__ void put_scale(const Fp8View& f, int64_t row, int64_t
 // T: float, bf16_t, or uint8_t for a matrix that is held in 8 bits.
 template <class T, bool FAR>
 __global__ __launch_bounds__(512) void quantize_tile_kernel(Source src, int32_t rows, int32_t cols,
-                                                            int32_t tiles_r, int32_t tiles_c, int32_t block,
-                                                            Fp8View by_rows, Fp8View by_cols) {
+                                                            int32_t tiles_r, int32_t tiles_c, uint32_t first_wg,
+                                                            int32_t block, Fp8View by_rows, Fp8View by_cols) {
     constexpr bool kHeld = sizeof(T) == 1;
     __shared__ __align__(16) uint8_t tile[128 * 128];
     __shared__ uint32_t top[8][128];
     __shared__ __align__(16) float inverse[128];
     __shared__ float rest[kHeld ? 128 : 1];
     const int t = threadIdx.x, cg = t & 15, rg = t >> 4, wave = t >> 6;
-    const int64_t rb = blockIdx.x / static_cast<uint32_t>(tiles_c);
-    const int32_t cb = static_cast<int32_t>(blockIdx.x - rb * tiles_c);
+    const uint32_t at = first_wg + blockIdx.x;
+    const int64_t rb = at / static_cast<uint32_t>(tiles_c);
+    const int32_t cb = static_cast<int32_t>(at - rb * tiles_c);
     const int64_t r0 = rb * 128 + rg * 4;
     const int32_t c0 = cb * 128 + cg * 8;
 
@@ -240,9 +241,9 @@ __global__ __launch_bounds__(512) void quantize_tile_kernel(Source src, int32_t 
 // ---------------------------------------------------------------------------
 template <class T, bool FAR>
 __global__ __launch_bounds__(256) void dequantize_kernel(Fp8View in, T* out, int64_t ld, int32_t blocks,
-                                                         int64_t total) {
+                                                         int64_t total, int64_t first_wg) {
     const int lane = threadIdx.x & 15;
-    const int64_t first = blockIdx.x * int64_t(16 * kItems) + (threadIdx.x >> 4);
+    const int64_t first = (first_wg + blockIdx.x) * (16 * kItems) + (threadIdx.x >> 4);
     int64_t row = first / blocks;
     int32_t kb = static_cast<int32_t>(first - row * blocks);
     u32x2 q[kItems];
@@ -277,17 +278,17 @@ template <class T>
 int tile_launch(const QuantizeArgs& a, hipStream_t stream) {
     const int64_t tr = (int64_t(a.rows) + 127) / 128, tc = (int64_t(a.cols) + 127) / 128;
     const int32_t block = a.by_rows.q != nullptr ? a.by_rows.block : a.by_cols.block;
-    if (tr * tc > 0x7fffff) return hipErrorInvalidValue;   // 512 threads each: 2^32 a launch
     auto launch = [&]<bool FAR>(std::bool_constant<FAR>) {
-        quantize_tile_kernel<T, FAR><<<static_cast<uint32_t>(tr * tc), 512, 0, stream>>>(
-            Source{a.x, a.ld, a.in}, a.rows, a.cols, static_cast<int32_t>(tr), static_cast<int32_t>(tc), block,
-            a.by_rows, a.by_cols);
+        return in_launches(tr * tc, 512, [&](int64_t first, uint32_t wgs) {
+            quantize_tile_kernel<T, FAR><<<wgs, 512, 0, stream>>>(
+                Source{a.x, a.ld, a.in}, a.rows, a.cols, static_cast<int32_t>(tr), static_cast<int32_t>(tc),
+                static_cast<uint32_t>(first), block, a.by_rows, a.by_cols);
+        });
     };
     // (what is held in 8 bits is read as it was written, one way)
-    if constexpr (sizeof(T) == 1) launch(std::false_type());
-    else if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) launch(std::true_type());
-    else launch(std::false_type());
-    return hipGetLastError();
+    if constexpr (sizeof(T) == 1) return launch(std::false_type());
+    else if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) return launch(std::true_type());
+    else return launch(std::false_type());
 }
 
 template <class T>
@@ -296,14 +297,14 @@ int quantize_launch(const QuantizeArgs& a, hipStream_t stream) {
     const int32_t blocks = static_cast<int32_t>((int64_t(a.cols) + 127) / 128);
     const int64_t total = int64_t(a.rows) * blocks;
     const int64_t wgs = (total + 16 * kItems - 1) / (16 * kItems);
-    if (wgs > 0xffffff) return hipErrorInvalidValue;
     auto launch = [&]<bool FAR>(std::bool_constant<FAR>) {
-        quantize_rows_kernel<T, FAR><<<static_cast<uint32_t>(wgs), 256, 0, stream>>>(
-            static_cast<const T*>(a.x), a.ld, a.cols, blocks, total, a.by_rows);
+        return in_launches(wgs, 256, [&](int64_t first, uint32_t n) {
+            quantize_rows_kernel<T, FAR><<<n, 256, 0, stream>>>(static_cast<const T*>(a.x), a.ld, a.cols, blocks, total,
+                                                                first, a.by_rows);
+        });
     };
-    if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) launch(std::true_type());
-    else launch(std::false_type());
-    return hipGetLastError();
+    if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) return launch(std::true_type());
+    return launch(std::false_type());
 }
 
 template <class T>
@@ -311,14 +312,14 @@ int dequantize_launch(const Fp8View& in, T* out, int64_t ld, hipStream_t stream)
     const int32_t blocks = static_cast<int32_t>((int64_t(in.cols) + 127) / 128);
     const int64_t total = int64_t(in.rows) * blocks;
     const int64_t wgs = (total + 16 * kItems - 1) / (16 * kItems);
-    if (wgs > 0xffffff) return hipErrorInvalidValue;
     auto launch = [&]<bool FAR>(std::bool_constant<FAR>) {
-        dequantize_kernel<T, FAR><<<static_cast<uint32_t>(wgs), 256, 0, stream>>>(in, out, ld, blocks, total);
+        return in_launches(wgs, 256, [&](int64_t first, uint32_t n) {
+            dequantize_kernel<T, FAR><<<n, 256, 0, stream>>>(in, out, ld, blocks, total, first);
+        });
     };
     // (only the stores pass by the cache: what is held in 8 bits may have been written just before)
-    if (is_far(int64_t(in.rows) * in.cols * sizeof(T))) launch(std::true_type());
-    else launch(std::false_type());
-    return hipGetLastError();
+    if (is_far(int64_t(in.rows) * in.cols * sizeof(T))) return launch(std::true_type());
+    return launch(std::false_type());
 }
 
 }  // namespace

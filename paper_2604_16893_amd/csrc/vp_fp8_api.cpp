@@ -36,6 +36,13 @@ bool misaligned(const void* p, int64_t to) { return reinterpret_cast<uintptr_t>(
 
 bool dims_ok(int64_t v) { return v >= 0 && v <= VP_MAX_DIM; }
 
+// The conversions that work on tiles of 128 x 128 number them in 32 bits.
+int32_t check_tiles(int64_t rows, int64_t cols) {
+    if ((rows + 127) / 128 * ((cols + 127) / 128) > int64_t(UINT32_MAX))
+        return fail(VP_ERR_DIMS, "a matrix of more than 2^32 tiles of 128 x 128");
+    return VP_OK;
+}
+
 int32_t check_dtype(int32_t dtype) {
     if (dtype != VP_OUT_F32 && dtype != VP_OUT_BF16)
         return fail(VP_ERR_ARG, "the element type must be VP_OUT_F32 or VP_OUT_BF16");
@@ -139,6 +146,7 @@ int32_t vp_fp8_quantize(const void* x, int32_t x_dtype, int64_t rows, int64_t co
     if (by_cols != nullptr) VP_TRY(check_fp8(by_cols, "by_cols", cols, rows, &a.by_cols));
     if (by_rows != nullptr && by_cols != nullptr && by_rows->block != by_cols->block)
         return fail(VP_ERR_ARG, "by_rows and by_cols must have one block");
+    if (by_cols != nullptr || by_rows->block != 1) VP_TRY(check_tiles(rows, cols));
     if (rows == 0 || cols == 0) return done(0, "");
     return done(vp::launch_quantize(a, stream), "quantize launch");
 }
@@ -148,6 +156,7 @@ int32_t vp_fp8_transpose(const vp_fp8* in, const vp_fp8* out, hipStream_t stream
     VP_TRY(check_fp8(in, "in", -1, -1, &a.in));
     VP_TRY(check_fp8(out, "out", in->cols, in->rows, &a.by_cols));
     if (in->block != out->block) return fail(VP_ERR_ARG, "in and out must have one block");
+    VP_TRY(check_tiles(in->rows, in->cols));
     a.type = vp::In::fp8;
     a.rows = a.in.rows;
     a.cols = a.in.cols;
@@ -173,7 +182,9 @@ int32_t vp_fp8_matmul_workspace(int64_t m, int64_t n, int64_t k, int32_t out_dty
     if (!dims_ok(m) || !dims_ok(n) || !dims_ok(k))
         return fail(VP_ERR_DIMS, "m, n and k must lie in [0, VP_MAX_DIM]");
     if (k > VP_MAX_SUM) return fail(VP_ERR_DIMS, "k must be at most VP_MAX_SUM");
-    *workspace_bytes = vp::matmul_workspace(m, n, k, out_dtype == VP_OUT_BF16);
+    const int64_t need = vp::matmul_workspace(m, n, k, out_dtype == VP_OUT_BF16);
+    if (need < 0) return fail(VP_ERR_DIMS, "a result of more tiles than a launch takes");
+    *workspace_bytes = need;
     vp::set_error(VP_OK, "");
     return VP_OK;
 }
@@ -184,16 +195,17 @@ int32_t vp_fp8_matmul(const vp_fp8* a, const vp_fp8* b, void* out, int32_t out_d
     VP_TRY(check_dtype(out_dtype));
     VP_TRY(check_fp8(a, "a", -1, -1, &m.a));
     VP_TRY(check_fp8(b, "b", -1, a->cols, &m.b));
-    VP_TRY(check_dense(out, "out", out_dtype, a->rows, b->rows, ld));
     if (a->cols > VP_MAX_SUM)
         return fail(VP_ERR_DIMS, "a sum of %lld products, at most %lld", static_cast<long long>(a->cols),
                     static_cast<long long>(VP_MAX_SUM));
+    m.bf16 = out_dtype == VP_OUT_BF16;
+    const int64_t need = vp::matmul_workspace(a->rows, b->rows, a->cols, m.bf16);
+    if (need < 0) return fail(VP_ERR_DIMS, "a result of more tiles than a launch takes");
+    VP_TRY(check_dense(out, "out", out_dtype, a->rows, b->rows, ld));
     m.out = out;
     m.ld = ld;
-    m.bf16 = out_dtype == VP_OUT_BF16;
     m.partial = static_cast<float*>(workspace);
-    VP_TRY(check_workspace(workspace, workspace_bytes,
-                           vp::matmul_workspace(a->rows, b->rows, a->cols, m.bf16)));
+    VP_TRY(check_workspace(workspace, workspace_bytes, need));
     if (a->rows == 0 || b->rows == 0) return done(0, "");
     return done(vp::launch_matmul(m, stream), "matmul launch");
 }

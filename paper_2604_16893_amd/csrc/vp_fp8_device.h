@@ -209,6 +209,18 @@ __device__ __forceinline__ float sum64(float v) {
     return v + __shfl_xor(v, 32);
 }
 
+// A launch has less than 2^32 threads: `total` workgroups of `threads` each, in as many launches as that takes.
+template <class F>
+int in_launches(int64_t total, int threads, F&& launch) {
+    const int64_t most = 0xffffffff / threads;
+    for (int64_t first = 0; first < total; first += most) {
+        launch(first, static_cast<uint32_t>(total - first < most ? total - first : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 // Whether bytes read once, or results that a later launch reads, are found no
 // sooner for having been kept: the memory-side cache holds 256 MB.  28,160 x 4096
 // in bf16, twice: norm 126 us nontemporal, 153 otherwise; 28,160 x 1280: 47 either

@@ -825,7 +825,8 @@ TileArgs tile_args(const MatmulArgs& a, int rows_m, int rows_n) {
 }
 
 // How a product is cut: tiles of 64 F x 64 F with the sum in `splits` pieces,
-// or F = 0: 16 FM x 16 FN by waves that split the sum among them.
+// or F = 0: 16 FM x 16 FN by waves that split the sum among them; F < 0: more
+// tiles than a launch takes.
 struct Cut {
     int f, fm, fn, splits;
 };
@@ -850,13 +851,15 @@ Cut choose(int64_t m, int64_t n, int64_t k, bool f8) {
                               {2, 512, 0.65, 1.08, 1.0, 1.77, 3.0},
                               {1, 512, 0.34, 0.47, 0.5, 0.68, 2.5}};
     const int64_t nk = (k + 127) / 128;
-    Cut best{1, 0, 0, 1};
+    Cut best{-1, 0, 0, 1};
     double least = 1e300;
     for (const Tile& t : tiles) {
         if ((t.f == 4 && nk < 4) || 64 * t.f * nk * 128 >= (int64_t(1) << 32)) continue;
         const int64_t count = ((m + 64 * t.f - 1) / (64 * t.f)) * ((n + 64 * t.f - 1) / (64 * t.f));
-        for (int s = 1; s <= 16 && s <= nk; s = s < 4 ? s + 1 : s + 2) {
+        for (int s = 1; s <= 16 && (s == 1 || s <= nk); s = s < 4 ? s + 1 : s + 2) {
             const int64_t per = (nk + s - 1) / s, wgs = count * s;
+            // workgroups of 256 threads in a launch (tiles of 256 may go to tiles of 128, four for each)
+            if (wgs > (t.f == 4 ? 0x3fffff : 0xffffff)) continue;
             if (s > 1 && (per < 4 || (s - 1) * per + 2 > nk)) continue;   // two blocks at least in every piece
             const double step = wgs <= (t.f == 4 ? 128 : 256) ? (f8 ? t.alone8 : t.alone32) : (f8 ? t.full8 : t.full32);
             const double rounds = static_cast<double>((wgs + t.slots - 1) / t.slots);
@@ -892,7 +895,6 @@ template <bool F8, class Out, int F, int SLOTS>
 int tile_launch(const MatmulArgs& a, int splits, hipStream_t stream) {
     TileArgs p = tile_args(a, 64 * F, 64 * F);
     const int64_t tiles = int64_t(p.tiles_m) * p.tiles_n;
-    if (tiles * splits > 0xffffff) return hipErrorInvalidValue;
     if (splits == 1) {
         tile_kernel<F8, Out, F, F, SLOTS><<<static_cast<uint32_t>(tiles), 256, 0, stream>>>(p);
         return hipGetLastError();
@@ -913,7 +915,6 @@ int big_launch(const MatmulArgs& a, int splits, hipStream_t stream) {
     if (splits == 1 && a.b.rows % (16 / sizeof(Out)) != 0) main.b.rows = a.b.rows / 256 * 256;
     TileArgs p = tile_args(main, 256, 256);
     const int64_t items = int64_t(p.tiles_m) * p.tiles_n * splits;
-    if (items > 0xffffff) return hipErrorInvalidValue;
     const uint32_t wgs = static_cast<uint32_t>(items < 256 ? items : 256);
     if (splits > 1) {
         p.out = a.partial;
@@ -938,7 +939,6 @@ template <bool F8, class Out, int FM, int FN>
 int wave_launch(const MatmulArgs& a, hipStream_t stream) {
     const TileArgs p = tile_args(a, 16 * FM, 16 * FN);
     const int64_t tiles = int64_t(p.tiles_m) * p.tiles_n;
-    if (tiles > 0x7fffff) return hipErrorInvalidValue;
     wave_kernel<F8, Out, FM, FN, 8><<<static_cast<uint32_t>(tiles), 512, 0, stream>>>(p);
     return hipGetLastError();
 }
@@ -965,6 +965,7 @@ int matmul_launch(const MatmulArgs& a, hipStream_t stream) {
 
 int64_t matmul_workspace(int64_t m, int64_t n, int64_t k, bool bf16) {
     const Cut c = choose(m, n, k, bf16);
+    if (c.f < 0) return -1;
     return c.splits > 1 ? c.splits * m * partial_ld(n) * 4 : 0;
 }
 
