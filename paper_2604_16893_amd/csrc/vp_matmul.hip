@@ -765,22 +765,6 @@ __global__ __launch_bounds__(64 * W) void wave_kernel(TileArgs p) {
     }
 }
 
-template <bool F8, class Out, int FM, int FN, int W>
-int wave_launch(const MatmulArgs& a, hipStream_t stream) {
-    TileArgs p{};
-    p.a = a.a;
-    p.b = a.b;
-    p.out = a.out;
-    p.ld = a.ld;
-    p.tiles_m = static_cast<int32_t>((int64_t(a.a.rows) + 16 * FM - 1) / (16 * FM));
-    p.tiles_n = static_cast<int32_t>((int64_t(a.b.rows) + 16 * FN - 1) / (16 * FN));
-    p.blocks = static_cast<int32_t>(a.a.ld / kBlock);
-    const int64_t tiles = int64_t(p.tiles_m) * p.tiles_n;
-    if (tiles > 0x3fffff) return hipErrorInvalidValue;
-    wave_kernel<F8, Out, FM, FN, W><<<static_cast<uint32_t>(tiles), 64 * W, 0, stream>>>(p);
-    return hipGetLastError();
-}
-
 // Rows of the splits' floats are whole eights apart.
 constexpr int64_t partial_ld(int64_t cols) { return (cols + 7) / 8 * 8; }
 
