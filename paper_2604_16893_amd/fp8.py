@@ -7,6 +7,11 @@ buffers and a stream; the others allocate their outputs with torch and run on
 the current stream.  Nothing here computes: every call is one native entry.
 Dense matrices are CUDA tensors [rows, cols] of float32 or bfloat16 whose rows
 are contiguous (any distance between rows).
+
+No function records a graph for torch.autograd: the gradients are calls of
+their own.  A forward call on a tensor that requires a gradient, where
+gradients are being recorded, is refused; under torch.no_grad(), and so in the
+forward method of a torch.autograd.Function, it is not.
 """
 from __future__ import annotations
 
@@ -169,6 +174,15 @@ def _vector(t, name: str, dtype, n: int):
     return t.data_ptr()
 
 
+def _no_graph(*tensors):
+    """Refuses what a graph would have to be recorded for."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                _bad("a tensor requires a gradient, and no graph is recorded here: call under torch.no_grad() (the gradients "
+                     "are calls of their own) or on its detach()")
+
+
 def _same_device(device: int, *others):
     """Every tensor on the current device, where the kernels run."""
     if device != torch._C._cuda_getDevice():
@@ -206,6 +220,7 @@ def vp_fp8_layout(rows: int, cols: int, block: int = 1):
 
 def vp_fp8_quantize(x, by_rows=None, by_cols=None, stream=None):
     """x [rows, cols] into 8 bits: by_rows Fp8 [rows, cols] and / or by_cols Fp8 [cols, rows], the transpose."""
+    _no_graph(x)
     ptr, ld = _dense(x, "x")
     device = _same_device(x.get_device(), by_rows, by_cols)
     rows, cols = x.shape
@@ -251,6 +266,7 @@ def vp_fp8_matmul(a: Fp8, b: Fp8, out, workspace=None, stream=None):
 def vp_rms_norm(x, weight, residual=None, eps: float = 1e-6, h=None, out=None, out8=None, rstd=None, stream=None):
     """h = x + residual, out / out8 = h * rstd * weight, rstd = 1 / sqrt(mean(h^2) + eps); outputs that are None
     are not written."""
+    _no_graph(x, weight, residual)
     px, ldx = _dense(x, "x")
     dtype = x.dtype
     rows, cols = x.shape
@@ -307,6 +323,7 @@ def fp8_quantize(x, block: int = 1, rows: bool = True, cols: bool = False):
     """x [M, K] in 8 bits: as it lies (rows), transposed (cols: Fp8 [K, M], blocks along M), or both, as a pair."""
     if not (rows or cols):
         _bad("neither rows nor cols")
+    _no_graph(x)
     ptr, ld = _dense(x, "x")
     m, k = x.shape
     device = _same_device(x.get_device())
@@ -359,6 +376,7 @@ def rms_norm(x, weight, residual=None, eps: float = 1e-6, out=None):
     as an Fp8 that fp8_matmul takes."""
     if out not in (None, "fp8"):
         _bad(f"unknown output {out!r}: None (x's type) or 'fp8'")
+    _no_graph(x, weight, residual)
     px, ldx = _dense(x, "x")
     dtype, where = x.dtype, x.device
     rows, cols = x.shape
