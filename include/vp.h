@@ -541,6 +541,26 @@ int32_t vp_fp8_matmul(const vp_fp8* a, const vp_fp8* b, void* out, int32_t out_d
                       void* workspace, int64_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Diagnostic: the kernel launches that vp_fp8_matmul makes for these sizes,
+ * without running them.  For tests and tuning.
+ * launches: HOST int32[capacity][4], or NULL with capacity 0.  Row i:
+ *   kind: VP_PRODUCT_TILES (workgroups with a tile of the result each),
+ *   VP_PRODUCT_WAVES (eight waves that share the sum of a smaller one) or
+ *   VP_PRODUCT_JOIN (the pieces' partial sums into the result);
+ *   rows and columns of a tile (0 for VP_PRODUCT_JOIN);
+ *   pieces that the sum over K is in.
+ *   Rows past `capacity` are not written.
+ * n_launches: HOST, receives the number of launches.
+ * Errors: as vp_fp8_matmul_workspace; VP_ERR_NULL (n_launches), VP_ERR_ARG
+ * (ld < n, capacity < 0, or launches NULL with capacity > 0).
+ */
+#define VP_PRODUCT_TILES 0
+#define VP_PRODUCT_WAVES 1
+#define VP_PRODUCT_JOIN 2
+int32_t vp_fp8_matmul_kernels(int64_t m, int64_t n, int64_t k, int32_t out_dtype, int64_t ld,
+                              int32_t* launches, int32_t capacity, int32_t* n_launches);
+
+/*
  * Root-mean-square norm of a residual stream, row by row:
  *   h = x + residual, rounded to dtype (h = x without a residual);
  *   rstd = 1 / sqrt(mean(h^2) + eps);   y = h * rstd * weight.

@@ -45,7 +45,7 @@ EXPORTED = ("vp_smart_resize_dims", "vp_sample_indices", "vp_filter_taps", "vp_f
             "vp_resize_layout", "vp_resize_kernels", "vp_resize_batch", "vp_position_ids", "vp_status_string",
             "vp_last_error_message", "vp_set_kernel_events",
             "vp_fp8_layout", "vp_fp8_quantize", "vp_fp8_transpose", "vp_fp8_dequantize",
-            "vp_fp8_matmul_workspace", "vp_fp8_matmul", "vp_rms_norm",
+            "vp_fp8_matmul_workspace", "vp_fp8_matmul", "vp_fp8_matmul_kernels", "vp_rms_norm",
             "vp_rms_norm_backward_workspace", "vp_rms_norm_backward")
 
 
@@ -513,7 +513,8 @@ def preprocess(items: Sequence, mean, std, out_dtype: str = "bf16", stream=None)
 # The 8-bit operators (products, norm, their gradients) load with their first use: they need torch, which the
 # host entry points above do not.
 _FP8 = ("Fp8", "VP_MAX_DIM", "VP_MAX_SUM", "vp_fp8", "vp_fp8_layout", "vp_fp8_quantize", "vp_fp8_transpose", "vp_fp8_dequantize",
-        "vp_fp8_matmul_workspace", "vp_fp8_matmul", "vp_rms_norm", "vp_rms_norm_backward_workspace",
+        "vp_fp8_matmul_workspace", "vp_fp8_matmul", "vp_fp8_matmul_kernels", "VP_PRODUCT_TILES", "VP_PRODUCT_WAVES",
+        "VP_PRODUCT_JOIN", "vp_rms_norm", "vp_rms_norm_backward_workspace",
         "vp_rms_norm_backward", "fp8_quantize", "fp8_transpose", "fp8_dequantize", "fp8_matmul", "rms_norm",
         "rms_norm_backward")
 

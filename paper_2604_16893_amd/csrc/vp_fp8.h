@@ -76,6 +76,8 @@ struct MatmulArgs {
 };
 // Bytes; -1 where the result has more tiles than a launch takes.
 int64_t matmul_workspace(int64_t m, int64_t n, int64_t k, bool bf16);
+// The launches of launch_matmul for these sizes, as vp_fp8_matmul_kernels gives them, and how many (2 at most).
+int describe_matmul(int64_t m, int64_t n, int64_t k, int64_t ld, bool bf16, int32_t (*rows)[4]);
 int launch_matmul(const MatmulArgs& a, hipStream_t stream);
 
 }  // namespace vp

@@ -7,6 +7,7 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <cstring>
 
 #include "vp.h"
 #include "vp_fp8.h"
@@ -208,6 +209,23 @@ int32_t vp_fp8_matmul(const vp_fp8* a, const vp_fp8* b, void* out, int32_t out_d
     VP_TRY(check_workspace(workspace, workspace_bytes, need));
     if (a->rows == 0 || b->rows == 0) return done(0, "");
     return done(vp::launch_matmul(m, stream), "matmul launch");
+}
+
+int32_t vp_fp8_matmul_kernels(int64_t m, int64_t n, int64_t k, int32_t out_dtype, int64_t ld, int32_t* launches,
+                              int32_t capacity, int32_t* n_launches) {
+    if (n_launches == nullptr) return fail(VP_ERR_NULL, "n_launches is NULL");
+    if (capacity < 0 || (launches == nullptr && capacity > 0))
+        return fail(VP_ERR_ARG, "launches must hold capacity rows of 4 int32");
+    int64_t need;
+    VP_TRY(vp_fp8_matmul_workspace(m, n, k, out_dtype, &need));
+    if (ld < n)
+        return fail(VP_ERR_ARG, "rows of %lld elements are %lld apart", static_cast<long long>(n),
+                    static_cast<long long>(ld));
+    int32_t rows[2][4];
+    const int count = vp::describe_matmul(m, n, k, ld, out_dtype == VP_OUT_BF16, rows);
+    for (int i = 0; i < count && i < capacity; ++i) std::memcpy(launches + 4 * i, rows[i], sizeof rows[i]);
+    *n_launches = count;
+    return VP_OK;
 }
 
 int32_t vp_rms_norm(const void* x, int64_t ldx, const void* residual, int64_t ldr,

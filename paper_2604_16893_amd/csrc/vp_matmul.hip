@@ -8,6 +8,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "vp.h"
 #include "vp_fp8_device.h"
 
 namespace vp {
@@ -867,6 +868,19 @@ Cut choose(int64_t m, int64_t n, int64_t k, bool f8) {
     return best;
 }
 
+// The same for a result whose rows are ld apart: a descriptor of the widest tiles' stores spans a tile's rows of it.
+Cut cut_for(int64_t m, int64_t n, int64_t k, int64_t ld, bool f8) {
+    Cut c = choose(m, n, k, f8);
+    if (c.f == 4 && (ld >= (1 << 21) || n >= (1 << 21))) c.f = 2;
+    return c;
+}
+
+// The widest tiles store 16 bytes at a time: where the rows of the result are not whole pieces of 16 bytes, the columns
+// that they take, up to the last whole tile; tiles of 128 take the rest.  (What the workspace holds is padded.)
+int64_t wide_columns(int64_t n, int splits, int size) {
+    return splits == 1 && n % (16 / size) != 0 ? n / 256 * 256 : n;
+}
+
 // Rows [n, rows) of a matrix; n a multiple of 128.
 Fp8View rows_from(Fp8View f, int32_t n) {
     f.q += n * f.ld;
@@ -891,12 +905,11 @@ int tile_launch(const MatmulArgs& a, int splits, hipStream_t stream) {
     return join_launch(a, static_cast<Out*>(a.out), splits, stream);
 }
 
-// Tiles of 256, one workgroup a CU.  Its stores are of 16 bytes: where the rows
-// of the result are not, the columns past the last whole tile go to tiles of 128.
+// Tiles of 256, one workgroup a CU.
 template <bool F8, class Out>
 int big_launch(const MatmulArgs& a, int splits, hipStream_t stream) {
     MatmulArgs main = a;
-    if (splits == 1 && a.b.rows % (16 / sizeof(Out)) != 0) main.b.rows = a.b.rows / 256 * 256;
+    main.b.rows = static_cast<int32_t>(wide_columns(a.b.rows, splits, sizeof(Out)));
     TileArgs p = tile_args(main, 256, 256);
     const int64_t items = int64_t(p.tiles_m) * p.tiles_n * splits;
     const uint32_t wgs = static_cast<uint32_t>(items < 256 ? items : 256);
@@ -929,12 +942,9 @@ int wave_launch(const MatmulArgs& a, hipStream_t stream) {
 
 template <bool F8, class Out>
 int matmul_launch(const MatmulArgs& a, hipStream_t stream) {
-    const Cut c = choose(a.a.rows, a.b.rows, a.a.cols, F8);
+    const Cut c = cut_for(a.a.rows, a.b.rows, a.a.cols, a.ld, F8);
     switch (c.f) {
-        case 4:
-            // (a descriptor spans a tile's rows of the result)
-            if (a.ld < (1 << 21) && a.b.rows < (1 << 21)) return big_launch<F8, Out>(a, c.splits, stream);
-            [[fallthrough]];
+        case 4: return big_launch<F8, Out>(a, c.splits, stream);
         case 2: return tile_launch<F8, Out, 2, 4>(a, c.splits, stream);
         case 1: return tile_launch<F8, Out, 1, 8>(a, c.splits, stream);
         default:
@@ -951,6 +961,26 @@ int64_t matmul_workspace(int64_t m, int64_t n, int64_t k, bool bf16) {
     const Cut c = choose(m, n, k, bf16);
     if (c.f < 0) return -1;
     return c.splits > 1 ? c.splits * m * partial_ld(n) * 4 : 0;
+}
+
+int describe_matmul(int64_t m, int64_t n, int64_t k, int64_t ld, bool bf16, int32_t (*rows)[4]) {
+    if (m == 0 || n == 0) return 0;
+    const Cut c = cut_for(m, n, k, ld, bf16);
+    int count = 0;
+    const auto add = [&](int32_t kind, int32_t tile_m, int32_t tile_n, int32_t pieces) {
+        const int32_t row[4] = {kind, tile_m, tile_n, pieces};
+        for (int i = 0; i < 4; ++i) rows[count][i] = row[i];
+        ++count;
+    };
+    if (c.f == 0) {
+        add(VP_PRODUCT_WAVES, 16 * c.fm, 16 * c.fn, 1);
+    } else {
+        const int64_t wide = c.f == 4 ? wide_columns(n, c.splits, bf16 ? 2 : 4) : n;
+        if (wide > 0) add(VP_PRODUCT_TILES, 64 * c.f, 64 * c.f, c.splits);
+        if (wide < n) add(VP_PRODUCT_TILES, 128, 128, 1);
+        if (c.splits > 1) add(VP_PRODUCT_JOIN, 0, 0, c.splits);
+    }
+    return count;
 }
 
 int launch_matmul(const MatmulArgs& a, hipStream_t stream) {

@@ -18,12 +18,14 @@ from __future__ import annotations
 import ctypes
 import functools
 
+import numpy as np
 import torch
 
 from . import VP_ERR_ARG, VP_ERR_DIMS, VP_OK, VP_OUT_BF16, VP_OUT_F32, VPError, _check, _stream_handle, lib
 
 VP_MAX_DIM = 0x7fffff00
 VP_MAX_SUM = 0x3ffff80
+VP_PRODUCT_TILES, VP_PRODUCT_WAVES, VP_PRODUCT_JOIN = 0, 1, 2
 _TYPES = {torch.float32: VP_OUT_F32, torch.bfloat16: VP_OUT_BF16}
 _NAMES = {"bf16": torch.bfloat16, "f32": torch.float32, torch.bfloat16: torch.bfloat16, torch.float32: torch.float32}
 _Q = torch.float8_e4m3fn
@@ -44,6 +46,7 @@ ARGTYPES = {
     "vp_fp8_dequantize": [_fp8p, _p, _i32, _i64, _p],
     "vp_fp8_matmul_workspace": [_i64, _i64, _i64, _i32, ctypes.POINTER(_i64)],
     "vp_fp8_matmul": [_fp8p, _fp8p, _p, _i32, _i64, _p, _i64, _p],
+    "vp_fp8_matmul_kernels": [_i64, _i64, _i64, _i32, _i64, ctypes.POINTER(_i32), _i32, ctypes.POINTER(_i32)],
     "vp_rms_norm": [_p, _i64, _p, _i64, _p, _i32, _i64, _i64, _f32, _p, _i64, _p, _i64, _fp8p, _p, _p],
     "vp_rms_norm_backward_workspace": [_i64, _i64, ctypes.POINTER(_i64)],
     "vp_rms_norm_backward": [_p, _i64, _p, _i64, _p, _p, _p, _i64, _i32, _i64, _i64, _p, _i64, _p, _p, _i64, _p],
@@ -261,6 +264,15 @@ def vp_fp8_matmul(a: Fp8, b: Fp8, out, workspace=None, stream=None):
                                _stream(stream, _same_device(a._device, b, out, workspace)))
     if st:
         _check(st, "vp_fp8_matmul")
+
+
+def vp_fp8_matmul_kernels(m: int, n: int, k: int, out_dtype: int = VP_OUT_BF16, ld=None):
+    """The launches vp_fp8_matmul makes for these sizes, as int32 rows (kind, tile rows, tile columns, pieces of the sum);
+    no kernel runs."""
+    rows, count = (_i32 * 8)(), _i32()
+    _check(_native.vp_fp8_matmul_kernels(m, n, k, out_dtype, n if ld is None else ld, rows, 2, ctypes.byref(count)),
+           "vp_fp8_matmul_kernels")
+    return np.array(rows, np.int32).reshape(2, 4)[:count.value]
 
 
 def vp_rms_norm(x, weight, residual=None, eps: float = 1e-6, h=None, out=None, out8=None, rstd=None, stream=None):
