@@ -285,10 +285,7 @@ int tile_launch(const QuantizeArgs& a, hipStream_t stream) {
                 static_cast<uint32_t>(first), block, a.by_rows, a.by_cols);
         });
     };
-    // (what is held in 8 bits is read as it was written, one way)
-    if constexpr (sizeof(T) == 1) return launch(std::false_type());
-    else if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) return launch(std::true_type());
-    else return launch(std::false_type());
+    return past_cache<T>(int64_t(a.rows) * a.cols * sizeof(T), launch);   // (what is held in 8 bits is read one way)
 }
 
 template <class T>
@@ -303,8 +300,7 @@ int quantize_launch(const QuantizeArgs& a, hipStream_t stream) {
                                                                 first, a.by_rows);
         });
     };
-    if (is_far(int64_t(a.rows) * a.cols * sizeof(T))) return launch(std::true_type());
-    return launch(std::false_type());
+    return past_cache<T>(int64_t(a.rows) * a.cols * sizeof(T), launch);
 }
 
 template <class T>
@@ -318,8 +314,7 @@ int dequantize_launch(const Fp8View& in, T* out, int64_t ld, hipStream_t stream)
         });
     };
     // (only the stores pass by the cache: what is held in 8 bits may have been written just before)
-    if (is_far(int64_t(in.rows) * in.cols * sizeof(T))) return launch(std::true_type());
-    return launch(std::false_type());
+    return past_cache<T>(int64_t(in.rows) * in.cols * sizeof(T), launch);
 }
 
 }  // namespace

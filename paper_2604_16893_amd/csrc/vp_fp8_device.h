@@ -3,6 +3,7 @@
 #pragma once
 
 #include <cstdint>
+#include <type_traits>
 
 #include <hip/hip_runtime.h>
 
@@ -39,16 +40,14 @@ struct Raw8<bf16_t> {
     bf16x8 a;
 };
 // FAR: the launch reads or writes more than the memory-side cache keeps, so its
-// lines are not kept for anyone (nontemporal).
+// lines are not kept for anyone (nontemporal).  bf16 alone: eight floats are two
+// pieces of 16 bytes a lane, half a line of every second lane's each, and past
+// the cache a half line costs a whole one.
 template <bool FAR>
 __device__ __forceinline__ void load_whole(const float* p, Raw8<float>& r) {
-    if constexpr (FAR) {
-        r.a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p));
-        r.b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p + 4));
-    } else {
-        r.a = *reinterpret_cast<const f32x4_any*>(p);
-        r.b = *reinterpret_cast<const f32x4_any*>(p + 4);
-    }
+    static_assert(!FAR);
+    r.a = *reinterpret_cast<const f32x4_any*>(p);
+    r.b = *reinterpret_cast<const f32x4_any*>(p + 4);
 }
 template <bool FAR>
 __device__ __forceinline__ void load_whole(const bf16_t* p, Raw8<bf16_t>& r) {
@@ -106,15 +105,10 @@ __device__ __forceinline__ void load8(const T* p, int64_t left, float (&v)[8]) {
 // Stores round to nearest even.
 template <bool FAR = false>
 __device__ __forceinline__ void store8(float* p, int64_t left, const float (&v)[8]) {
+    static_assert(!FAR);
     if (left >= 8) {
-        const f32x4 a{v[0], v[1], v[2], v[3]}, b{v[4], v[5], v[6], v[7]};
-        if constexpr (FAR) {
-            __builtin_nontemporal_store(a, reinterpret_cast<f32x4_any*>(p));
-            __builtin_nontemporal_store(b, reinterpret_cast<f32x4_any*>(p + 4));
-        } else {
-            *reinterpret_cast<f32x4_any*>(p) = a;
-            *reinterpret_cast<f32x4_any*>(p + 4) = b;
-        }
+        *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4_any*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -222,9 +216,20 @@ int in_launches(int64_t total, int threads, F&& launch) {
 }
 
 // Whether bytes read once, or results that a later launch reads, are found no
-// sooner for having been kept: the memory-side cache holds 256 MB.  28,160 x 4096
-// in bf16, twice: norm 126 us nontemporal, 153 otherwise; 28,160 x 1280: 47 either
-// way; rows of 8192 x 8192 into 8 bits: 34 and 32.
+// sooner for having been kept: the memory-side cache holds 256 MB.  In us, past the
+// cache and through it: norm of 28,160 x 4096 in bf16 with a residual to 8 bits 149
+// and 154, its gradients 157 and 173; dequantise to bf16 50 and 63; 28,160 x 1280
+// and shorter within 1 either way.
 inline bool is_far(int64_t bytes) { return bytes > int64_t(200) << 20; }
+
+// launch(FAR) for elements of T.  In f32 the same norm takes 323 past the cache and
+// 277 through it, its gradients 382 and 350, dequantise 189 and 142, quantise 110 and
+// 106, both forms 148 and 135.
+template <class T, class F>
+int past_cache(int64_t bytes, F&& launch) {
+    if constexpr (sizeof(T) == 2)
+        if (is_far(bytes)) return launch(std::true_type());
+    return launch(std::false_type());
+}
 
 }  // namespace vp

@@ -387,7 +387,7 @@ uint32_t backward_groups(int64_t rows, int64_t cols) {
 }
 
 template <class T, bool FAR>
-void norm_rows(const NormArgs& a, hipStream_t s) {
+int norm_rows(const NormArgs& a, hipStream_t s) {
     const uint32_t g = groups_of(a.rows, by_wave(a.rows, a.cols), kMostGroups);
     if (by_wave(a.rows, a.cols)) {
         if (a.cols <= 512) norm_kernel<T, 64, 1, FAR><<<g, 256, 0, s>>>(a);
@@ -397,15 +397,17 @@ void norm_rows(const NormArgs& a, hipStream_t s) {
     else if (a.cols <= 4096) norm_kernel<T, 256, 2, FAR><<<g, 256, 0, s>>>(a);
     else if (a.cols <= 6144) norm_kernel<T, 256, 3, FAR><<<g, 256, 0, s>>>(a);
     else norm_kernel<T, 256, 4, FAR><<<g, 256, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 template <class T>
 int norm_launch(const NormArgs& a, hipStream_t s) {
+    if (is_long(a.cols)) {
+        norm_long_kernel<T><<<groups_of(a.rows, by_wave(a.rows, a.cols), kMostGroups), 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
     const int64_t reads = int64_t(a.rows) * a.cols * sizeof(T) * (a.residual != nullptr ? 2 : 1);
-    if (is_long(a.cols)) norm_long_kernel<T><<<groups_of(a.rows, by_wave(a.rows, a.cols), kMostGroups), 256, 0, s>>>(a);
-    else if (is_far(reads)) norm_rows<T, true>(a, s);
-    else norm_rows<T, false>(a, s);
-    return hipGetLastError();
+    return past_cache<T>(reads, [&]<bool FAR>(std::bool_constant<FAR>) { return norm_rows<T, FAR>(a, s); });
 }
 
 uint32_t across(int64_t cols, int64_t each) {
@@ -414,7 +416,7 @@ uint32_t across(int64_t cols, int64_t each) {
 }
 
 template <class T, bool FAR>
-void norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
+int norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
     const bool wave = backward_by_wave(a.rows, a.cols);
     const uint32_t g = backward_groups(a.rows, a.cols);
     if (wave) {
@@ -424,23 +426,21 @@ void norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
     else if (a.cols <= 4096) norm_backward_kernel<T, 256, 2, FAR><<<g, 256, 0, s>>>(a);
     else if (a.cols <= 6144) norm_backward_kernel<T, 256, 3, FAR><<<g, 256, 0, s>>>(a);
     else norm_backward_kernel<T, 256, 4, FAR><<<g, 256, 0, s>>>(a);
+    return hipGetLastError();
 }
 
 template <class T>
 int norm_backward_launch(const NormBackwardArgs& a, hipStream_t s) {
     const int groups = norm_backward_groups(a.rows, a.cols);
-    if (a.rows > 0) {
-        const int64_t reads = int64_t(a.rows) * a.cols * sizeof(T) * (a.dh != nullptr ? 3 : 2);
-        if (is_long(a.cols)) {
-            if (a.partial != nullptr)
-                norm_dweight_long_kernel<T><<<dim3(across(a.cols, 64), static_cast<uint32_t>(groups)), 256, 0, s>>>(a);
-            norm_backward_long_kernel<T><<<groups_of(a.rows, false, kMostGroups), 256, 0, s>>>(a);
-        } else if (is_far(reads)) {
-            norm_backward_rows<T, true>(a, s);
-        } else {
-            norm_backward_rows<T, false>(a, s);
-        }
+    if (a.rows > 0 && is_long(a.cols)) {
+        if (a.partial != nullptr)
+            norm_dweight_long_kernel<T><<<dim3(across(a.cols, 64), static_cast<uint32_t>(groups)), 256, 0, s>>>(a);
+        norm_backward_long_kernel<T><<<groups_of(a.rows, false, kMostGroups), 256, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    } else if (a.rows > 0) {
+        const int64_t reads = int64_t(a.rows) * a.cols * sizeof(T) * (a.dh != nullptr ? 3 : 2);
+        const int e = past_cache<T>(reads, [&]<bool FAR>(std::bool_constant<FAR>) { return norm_backward_rows<T, FAR>(a, s); });
         if (e != hipSuccess) return e;
     }
     if (a.dweight != nullptr && groups == 0) {
