@@ -63,8 +63,8 @@ struct NormBackwardArgs {
     int64_t ldy, ldh, lddh, lddx;
     int32_t rows, cols;
 };
-// Rows of partial sums that the launch writes for this shape.
-int norm_backward_groups(int64_t rows, int64_t cols);
+// Rows of partial sums that the launch writes for this shape and elements of `size` bytes; bf16 has the most.
+int norm_backward_groups(int64_t rows, int64_t cols, int size = 2);
 int launch_norm_backward(const NormBackwardArgs& a, bool bf16, hipStream_t stream);
 
 struct MatmulArgs {

@@ -359,17 +359,24 @@ __global__ __launch_bounds__(256) void zero_kernel(float* dweight, int32_t cols)
     if (c < cols) dweight[c] = 0.0f;
 }
 
-// A row's threads: a wave up to 2048 columns where there are rows enough to
-// fill the chip with waves (28,160 x 1280: 47.5 us against 61.5), a workgroup
-// otherwise, with one vector a lane for each 2048 columns up to 8192 (4000 x 5120
-// with three: 24.5 us against 27.1 with four, its gradients 32.0 against 34.7).
+// A row's threads: a wave up to 2048 columns in bf16, 1024 in f32, where there
+// are rows enough to fill the chip with waves, a workgroup otherwise, with one
+// vector a lane for each 2048 columns up to 8192 (4000 x 5120 with three: 24.5 us
+// against 27.1 with four, its gradients 32.0 against 34.7).  Kernel times in us, a
+// wave's and a workgroup's: bf16, 28,160 x 1280 45.4 and 51.2, 4096 x 1280 10.7 and
+// 11.2, 3000 x 1280 9.2 and 9.1, 1024 x 1280 6.6 and 5.1; f32, 28,160 x 2048 147 and
+// 138, 4096 x 1280 15.9 and 15.2, 4096 x 1000 11.7 and 12.4.  (Rows of up to 1024
+// columns gain by it sooner: 2048 x 1000 in bf16 5.7 and 7.0, in f32 7.2 and 7.1.)
 constexpr int kFewRows = 4096;
 
 bool is_long(int64_t cols) { return cols > 8192; }
-bool by_wave(int64_t rows, int64_t cols) { return cols <= 512 || (cols <= 2048 && rows >= kFewRows); }
-// The backward pass holds twice as much a row: up to 1024 columns (28,160 rows
-// of 1000 in 46 us against 74 by workgroups, of 1280 in 82 against 58).
-bool backward_by_wave(int64_t rows, int64_t cols) { return cols <= 1024 && by_wave(rows, cols); }
+bool by_wave(int64_t rows, int64_t cols, int size) {
+    return cols <= 512 || (cols <= (size == 2 ? 2048 : 1024) && rows >= kFewRows);
+}
+// The backward pass holds twice as much a row: up to 1024 columns (28,160 rows in
+// bf16, of 1000 in 40.1 us against 46.9 by workgroups, of 600 in 33.6 against 45.8;
+// 4096 x 1000 12.5 against 15.4, in f32 17.2 against 17.8).
+bool backward_by_wave(int64_t rows, int64_t cols) { return cols <= 1024 && by_wave(rows, cols, 4); }
 
 uint32_t groups_of(int64_t rows, bool wave, int64_t most) {
     const int64_t per = wave ? 4 : 1, g = (rows + per - 1) / per;
@@ -377,22 +384,26 @@ uint32_t groups_of(int64_t rows, bool wave, int64_t most) {
 }
 
 // A workgroup's share of dweight is a row of floats, written and read again, so
-// there are half as many as in the forward pass: 28,160 x 4096 in 156 us against
-// 171, 1024 x 8192 in 20 against 26, 3500 x 2048 in 14.4 against 15.7.  Shorter
-// rows need more of them under way once they are many: 28,160 x 1280 in 55 us
-// against 77 by 512 workgroups, x 1600 in 64 against 76, x 2048 in 85 against 76.
-uint32_t backward_groups(int64_t rows, int64_t cols) {
+// there are half as many as in the forward pass: 28,160 x 4096 in bf16 in 156 us
+// against 171, 1024 x 8192 in 20 against 26.  Shorter rows in bf16, 16 bytes a lane of
+// each input, need more of them under way once they are many; with 512 and 1024
+// workgroups: 28,160 x 1280 77.7 and 57.2, 10,000 x 1536 28.0 and 25.6, 3000 x 1280
+// 14.5 and 14.0, but 2048 x 1280 12.1 and 12.9, 28,160 x 2048 75.9 and 85.8, and in f32
+// 28,160 x 1280 112 and 116.
+uint32_t backward_groups(int64_t rows, int64_t cols, int size) {
     const bool wave = backward_by_wave(rows, cols);
-    return groups_of(rows, wave, !wave && cols <= 1792 && rows >= 2560 ? kMostGroups : kMostGroups / 2);
+    const bool more = size == 2 && !wave && cols <= 1792 && rows >= 2560;
+    return groups_of(rows, wave, more ? kMostGroups : kMostGroups / 2);
 }
 
 template <class T, bool FAR>
 int norm_rows(const NormArgs& a, hipStream_t s) {
-    const uint32_t g = groups_of(a.rows, by_wave(a.rows, a.cols), kMostGroups);
-    if (by_wave(a.rows, a.cols)) {
+    const bool wave = by_wave(a.rows, a.cols, sizeof(T));
+    const uint32_t g = groups_of(a.rows, wave, kMostGroups);
+    if (wave) {
         if (a.cols <= 512) norm_kernel<T, 64, 1, FAR><<<g, 256, 0, s>>>(a);
         else if (a.cols <= 1024) norm_kernel<T, 64, 2, FAR><<<g, 256, 0, s>>>(a);
-        else norm_kernel<T, 64, 4, FAR><<<g, 256, 0, s>>>(a);
+        else if constexpr (sizeof(T) == 2) norm_kernel<T, 64, 4, FAR><<<g, 256, 0, s>>>(a);
     } else if (a.cols <= 2048) norm_kernel<T, 256, 1, FAR><<<g, 256, 0, s>>>(a);
     else if (a.cols <= 4096) norm_kernel<T, 256, 2, FAR><<<g, 256, 0, s>>>(a);
     else if (a.cols <= 6144) norm_kernel<T, 256, 3, FAR><<<g, 256, 0, s>>>(a);
@@ -403,7 +414,7 @@ int norm_rows(const NormArgs& a, hipStream_t s) {
 template <class T>
 int norm_launch(const NormArgs& a, hipStream_t s) {
     if (is_long(a.cols)) {
-        norm_long_kernel<T><<<groups_of(a.rows, by_wave(a.rows, a.cols), kMostGroups), 256, 0, s>>>(a);
+        norm_long_kernel<T><<<groups_of(a.rows, false, kMostGroups), 256, 0, s>>>(a);
         return hipGetLastError();
     }
     const int64_t reads = int64_t(a.rows) * a.cols * sizeof(T) * (a.residual != nullptr ? 2 : 1);
@@ -418,7 +429,7 @@ uint32_t across(int64_t cols, int64_t each) {
 template <class T, bool FAR>
 int norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
     const bool wave = backward_by_wave(a.rows, a.cols);
-    const uint32_t g = backward_groups(a.rows, a.cols);
+    const uint32_t g = backward_groups(a.rows, a.cols, sizeof(T));
     if (wave) {
         if (a.cols <= 512) norm_backward_kernel<T, 64, 1, FAR><<<g, 256, 0, s>>>(a);
         else norm_backward_kernel<T, 64, 2, FAR><<<g, 256, 0, s>>>(a);
@@ -431,7 +442,7 @@ int norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
 
 template <class T>
 int norm_backward_launch(const NormBackwardArgs& a, hipStream_t s) {
-    const int groups = norm_backward_groups(a.rows, a.cols);
+    const int groups = norm_backward_groups(a.rows, a.cols, sizeof(T));
     if (a.rows > 0 && is_long(a.cols)) {
         if (a.partial != nullptr)
             norm_dweight_long_kernel<T><<<dim3(across(a.cols, 64), static_cast<uint32_t>(groups)), 256, 0, s>>>(a);
@@ -454,9 +465,9 @@ int norm_backward_launch(const NormBackwardArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int norm_backward_groups(int64_t rows, int64_t cols) {
+int norm_backward_groups(int64_t rows, int64_t cols, int size) {
     if (rows == 0) return 0;
-    if (!is_long(cols)) return static_cast<int>(backward_groups(rows, cols));
+    if (!is_long(cols)) return static_cast<int>(backward_groups(rows, cols, size));
     const int64_t g = (rows + 3) / 4;
     return static_cast<int>(g < kLongGroups ? g : kLongGroups);
 }
