@@ -15,6 +15,9 @@ namespace {
 
 constexpr int kMostGroups = 1024;   // workgroups of a launch: four a CU
 constexpr int kLongGroups = 32;     // of rows, for dweight of long rows
+// Rows that dweight adds in one sequence, then the parts.  (All of a wave's rows in one, 2^22 rows of 64 equal values came
+// out 1.7e-5 off, 2^26 rows 1.2e-4.)
+constexpr int kPart = 64;
 constexpr int64_t kMostAcross = 0xffff;   // workgroups across a row's columns: a launch has less than 2^32 threads
 
 // Sum over the NT threads of a row, the same in all of them.
@@ -185,7 +188,9 @@ __device__ __forceinline__ void load_row(const NormBackwardArgs& a, int64_t row,
 // too little under way: 28,160 x 1280 in 58.1 us against 77.6.  Wider rows lose
 // waves to the registers that it takes (4096: 162 us against 157), and rows of
 // one wave have other waves' loads beside theirs (768: 42.2 against 36.3).
-template <class T, int NT, int V, bool FAR>
+// MANY: a thread has more than kPart rows, and adds their dweight in parts.  (Compiled in, it costs launches of fewer
+// rows 2 to 3 %: 28,160 x 384 in 25.6 us against 24.8.)
+template <class T, int NT, int V, bool FAR, bool MANY>
 __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackwardArgs a) {
     constexpr bool AHEAD = NT == 256 && V == 1;
     __shared__ float shared[4];
@@ -193,6 +198,7 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackwardArgs a) 
     const int t = threadIdx.x % NT;
     const int64_t step = int64_t(gridDim.x) * (256 / NT);
     float w[V][8], dw[V][8];
+    float parts[NT == 64 ? V : 1][8];   // a wave's finished parts of dweight; a workgroup's are in `partial`
     Raw8<T> y[V], h[V], dh[V];
     float rstd = 0.0f;
     int64_t row = blockIdx.x * int64_t(256 / NT) + threadIdx.x / NT;
@@ -206,10 +212,43 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackwardArgs a) 
         const int64_t c = (k * NT + t) * 8;
         load8(static_cast<const T*>(a.weight) + c, a.cols - c, w[k]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[k][i] = 0.0f;
+        for (int i = 0; i < 8; ++i) {
+            dw[k][i] = 0.0f;
+            if constexpr (NT == 64) parts[k][i] = 0.0f;
+        }
     }
+    float* to = a.partial + blockIdx.x * int64_t(a.cols);
+    bool begun = false;
+    const auto end_part = [&]() {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const int64_t c = (k * NT + t) * 8;
+            if constexpr (NT != 64) {
+                if (MANY && begun) {
+                    float before[8];
+                    load8(to + c, a.cols - c, before);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dw[k][i] += before[i];
+                }
+                store8(to + c, a.cols - c, dw[k]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (NT == 64) parts[k][i] += dw[k][i];
+                dw[k][i] = 0.0f;
+            }
+        }
+        begun = true;
+    };
     if (AHEAD && row < a.rows) fetch(row);
-    for (; row < a.rows; row += step) {
+    for (int in_part = 0; row < a.rows; row += step) {
+        if (MANY) {
+            if (in_part == kPart) {
+                end_part();
+                in_part = 0;
+            }
+            ++in_part;
+        }
         if constexpr (!AHEAD) fetch(row);
         float g[V][8], n[V][8], sum = 0.0f;
         Raw8<T> add[V];
@@ -234,13 +273,13 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackwardArgs a) 
         for (int k = 0; k < V; ++k) write_dx<FAR, T>(a, row, (k * NT + t) * 8, r, mean, g[k], n[k], w[k], add[k]);
     }
     if (a.partial == nullptr) return;
-    float* to = a.partial + blockIdx.x * int64_t(a.cols);
+    end_part();
     if constexpr (NT == 64) {   // four waves, each with rows of its own
         const int wave = threadIdx.x >> 6;
 #pragma unroll
         for (int k = 0; k < V; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) join[(wave * V * 8 + k * 8 + i) * 64 + t] = dw[k][i];
+            for (int i = 0; i < 8; ++i) join[(wave * V * 8 + k * 8 + i) * 64 + t] = parts[k][i];
         __syncthreads();
         for (int e = wave; e < V * 8; e += 4) {
             const int64_t c = ((e / 8) * 64 + t) * 8 + e % 8;
@@ -248,12 +287,6 @@ __global__ __launch_bounds__(256) void norm_backward_kernel(NormBackwardArgs a) 
 #pragma unroll
             for (int u = 0; u < 4; ++u) s += join[(u * V * 8 + e) * 64 + t];
             if (c < a.cols) to[c] = s;
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const int64_t c = (k * NT + t) * 8;
-            store8(to + c, a.cols - c, dw[k]);
         }
     }
 }
@@ -297,11 +330,17 @@ __global__ __launch_bounds__(256) void norm_dweight_long_kernel(NormBackwardArgs
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int64_t c0 = blockIdx.x * int64_t(64); c0 < a.cols; c0 += gridDim.x * int64_t(64)) {
         const int64_t c = c0 + lane;
+        const int64_t step = gridDim.y * int64_t(4);
         float s = 0.0f;
         if (c < a.cols)
-            for (int64_t row = blockIdx.y * int64_t(4) + wave; row < a.rows; row += gridDim.y * int64_t(4))
-                s += static_cast<float>(static_cast<const T*>(a.dy)[row * a.ldy + c]) *
-                     (static_cast<float>(static_cast<const T*>(a.h)[row * a.ldh + c]) * a.rstd[row]);
+            for (int64_t row0 = blockIdx.y * int64_t(4) + wave; row0 < a.rows; row0 += kPart * step) {
+                const int64_t end = min(int64_t(a.rows), row0 + kPart * step);
+                float part = 0.0f;
+                for (int64_t row = row0; row < end; row += step)
+                    part += static_cast<float>(static_cast<const T*>(a.dy)[row * a.ldy + c]) *
+                            (static_cast<float>(static_cast<const T*>(a.h)[row * a.ldh + c]) * a.rstd[row]);
+                s += part;
+            }
         join[wave][lane] = s;
         __syncthreads();
         if (wave == 0 && c < a.cols)
@@ -426,17 +465,15 @@ uint32_t across(int64_t cols, int64_t each) {
     return static_cast<uint32_t>(n < kMostAcross ? n : kMostAcross);
 }
 
-template <class T, bool FAR>
-int norm_backward_rows(const NormBackwardArgs& a, hipStream_t s) {
-    const bool wave = backward_by_wave(a.rows, a.cols);
-    const uint32_t g = backward_groups(a.rows, a.cols, sizeof(T));
+template <class T, bool FAR, bool MANY>
+int norm_backward_rows(const NormBackwardArgs& a, bool wave, uint32_t g, hipStream_t s) {
     if (wave) {
-        if (a.cols <= 512) norm_backward_kernel<T, 64, 1, FAR><<<g, 256, 0, s>>>(a);
-        else norm_backward_kernel<T, 64, 2, FAR><<<g, 256, 0, s>>>(a);
-    } else if (a.cols <= 2048) norm_backward_kernel<T, 256, 1, FAR><<<g, 256, 0, s>>>(a);
-    else if (a.cols <= 4096) norm_backward_kernel<T, 256, 2, FAR><<<g, 256, 0, s>>>(a);
-    else if (a.cols <= 6144) norm_backward_kernel<T, 256, 3, FAR><<<g, 256, 0, s>>>(a);
-    else norm_backward_kernel<T, 256, 4, FAR><<<g, 256, 0, s>>>(a);
+        if (a.cols <= 512) norm_backward_kernel<T, 64, 1, FAR, MANY><<<g, 256, 0, s>>>(a);
+        else norm_backward_kernel<T, 64, 2, FAR, MANY><<<g, 256, 0, s>>>(a);
+    } else if (a.cols <= 2048) norm_backward_kernel<T, 256, 1, FAR, MANY><<<g, 256, 0, s>>>(a);
+    else if (a.cols <= 4096) norm_backward_kernel<T, 256, 2, FAR, MANY><<<g, 256, 0, s>>>(a);
+    else if (a.cols <= 6144) norm_backward_kernel<T, 256, 3, FAR, MANY><<<g, 256, 0, s>>>(a);
+    else norm_backward_kernel<T, 256, 4, FAR, MANY><<<g, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -451,7 +488,12 @@ int norm_backward_launch(const NormBackwardArgs& a, hipStream_t s) {
         if (e != hipSuccess) return e;
     } else if (a.rows > 0) {
         const int64_t reads = int64_t(a.rows) * a.cols * sizeof(T) * (a.dh != nullptr ? 3 : 2);
-        const int e = past_cache<T>(reads, [&]<bool FAR>(std::bool_constant<FAR>) { return norm_backward_rows<T, FAR>(a, s); });
+        const bool wave = backward_by_wave(a.rows, a.cols);
+        const uint32_t g = backward_groups(a.rows, a.cols, sizeof(T));
+        const bool many = a.partial != nullptr && a.rows > int64_t(g) * (wave ? 4 : 1) * kPart;
+        const int e = past_cache<T>(reads, [&]<bool FAR>(std::bool_constant<FAR>) {
+            return many ? norm_backward_rows<T, FAR, true>(a, wave, g, s) : norm_backward_rows<T, FAR, false>(a, wave, g, s);
+        });
         if (e != hipSuccess) return e;
     }
     if (a.dweight != nullptr && groups == 0) {
