@@ -4,10 +4,13 @@
 // squares and its output, so each input is read once: 8 columns in each of V
 // vectors a thread, NT threads a row (a wave for short rows, so that no row
 // waits at a barrier; 256 threads up to 8192 columns).  Longer rows are read
-// a second time, which finds them in L2.  Sums are in f32: V * 8 products in a
-// thread, then a tree over lanes and waves.  28,160 x 4096 in bf16: with a
-// residual, and h, to 8 bits 127 us, 6.4 TB/s; gradients 156 us, 6.1 TB/s and the
-// sum of the workgroups' shares.
+// a second time, from beyond L2, which does not hold the rows of 1024 workgroups
+// (4096 x 12,288 in bf16 with a residual: 401 MB read, 201 needed).  Sums are in
+// f32: V * 8 products in a thread, then a tree over lanes and waves.  28,160 x 4096
+// in bf16: with a residual, and h, to 8 bits 127 us, 6.4 TB/s; gradients 147 us, 6.3
+// TB/s, and the sum of the workgroups' shares, 4.5 us.  4096 x 12,288: 92 us, 6.0
+// TB/s of what is moved; gradients 84 us for dx, which reads dy and h twice, and 60
+// for dweight, which reads them once more.
 #include "vp_fp8_device.h"
 
 namespace vp {
@@ -401,8 +404,8 @@ __global__ __launch_bounds__(256) void zero_kernel(float* dweight, int32_t cols)
 // A row's threads: a wave up to 2048 columns in bf16, 1024 in f32, where there
 // are rows enough to fill the chip with waves, a workgroup otherwise, with one
 // vector a lane for each 2048 columns up to 8192 (4000 x 5120 with three: 24.5 us
-// against 27.1 with four, its gradients 32.0 against 34.7).  Kernel times in us, a
-// wave's and a workgroup's: bf16, 28,160 x 1280 45.4 and 51.2, 4096 x 1280 10.7 and
+// against 27.1 with four, its gradients 32.0 against 34.7).  Kernel times in us on
+// inputs that repeat, a wave's and a workgroup's: bf16, 28,160 x 1280 45.4 and 51.2, 4096 x 1280 10.7 and
 // 11.2, 3000 x 1280 9.2 and 9.1, 1024 x 1280 6.6 and 5.1; f32, 28,160 x 2048 147 and
 // 138, 4096 x 1280 15.9 and 15.2, 4096 x 1000 11.7 and 12.4.  (Rows of up to 1024
 // columns gain by it sooner: 2048 x 1000 in bf16 5.7 and 7.0, in f32 7.2 and 7.1.)

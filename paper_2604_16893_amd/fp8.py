@@ -369,7 +369,9 @@ def fp8_dequantize(src: Fp8, out_dtype="bf16"):
 def fp8_matmul(a: Fp8, b: Fp8, out_dtype="bf16"):
     """a [M, K] b [N, K]^T in bf16 or f32.  A linear layer: y = fp8_matmul(x, w); its gradients: dx =
     fp8_matmul(dy, fp8_transpose(w)), dw = fp8_matmul(dy_t, fp8_transpose(x), "f32") with
-    dy, dy_t = fp8_quantize(grad, cols=True)."""
+    dy, dy_t = fp8_quantize(grad, cols=True).  Results in f32 have sums in f32; those in bf16 are formed by the 8-bit
+    instructions, which lose the products below 2^-13 of the largest of 8 neighbours: fp8_matmul(a, b, "f32").bfloat16()
+    does not."""
     dtype = _dtype(out_dtype)
     device = _same_device(a._device, b)
     m, n, code, where = a.rows, b.rows, _TYPES[dtype], a.device

@@ -78,3 +78,22 @@ def test_product_of_large_and_small_scales(m, n, k, out):
     """Scales of 2^118 against 2^-120: values just below 2^128, products of order one."""
     a, b = held(m, k, (243, 244, 245), 1), held(n, k, (7, 8), 2, 128)
     check_product(vp.fp8_matmul(a, b, out), a, b, k)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 300, 640), (200, 2106, 1024), (66, 24628, 140), (130, 38488, 513)])
+@pytest.mark.parametrize("small", [0.171875, 0.1875, 1.0])
+def test_product_whose_large_terms_cancel(m, n, k, small):
+    """One product of 256 in each run of 8 columns, its sign turned over from run to run, and seven of small^2 beside it
+    (0.0295 is just below 2^-13 of 256).  f32 results hold the sum; bf16 ones may lose 7 * 2^-13 of each run's largest."""
+    r = torch.arange(k, device=DEV)
+    x = torch.where(r % 8 == 3, 16.0, small).repeat(m, 1)
+    y = torch.where(r % 8 == 3, torch.where(r // 8 % 2 == 0, 16.0, -16.0), small).repeat(n, 1)
+    a, b = vp.fp8_quantize(x), vp.fp8_quantize(y, 128)
+    va, vb = R.values(a.q, a.scale, k, 1), R.values(b.q, b.scale, k, 128)
+    assert torch.equal(va, x.double()) and torch.equal(vb, y.double())
+    ref = (va[0] * vb[0]).sum()
+    f32 = vp.fp8_matmul(a, b, "f32")
+    check_product(f32, a, b, k)
+    off = (vp.fp8_matmul(a, b).double() - ref).abs()
+    most = 7 * 2.0 ** -13 * 256 * R.up(k, 8) / 8 + k ** 0.5 * 2.0 ** -23 * (va[0] * vb[0]).abs().sum()
+    assert bool((off <= most * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs()).all())
