@@ -401,8 +401,9 @@ struct Piece {           // of the work: a tile, and of its sum blocks [first, f
 // a lane) at a time, one quarter ahead of the instructions: 16 x 32 cycles, in
 // which 32 conversions stand, so the registers hold two quarters widened.
 // FAR: the result is more than the memory-side cache keeps and does not go
-// through it (28,160 x 4096 x 1280 and the norm that reads the result: 204 us,
-// otherwise 220; results of 32 to 128 MiB 1 to 6 % slower for their reader).
+// through it (to bf16, 28,160 x 4096 x 1280 in 142 us, otherwise 151, 89,600 x 1280 x
+// 1536 in 174 and 190; to f32 the same alone, with the norm that reads the result 362
+// and 377; results of 32 to 128 MiB 1 to 6 % slower for their reader).
 template <class Out, bool F8, bool FAR>
 __global__ __launch_bounds__(256, 1) void big_kernel(TileArgs p, int32_t splits) {
     constexpr int kBytes = 256 * 128;                           // of an operand's block

@@ -7,8 +7,8 @@
 // a second time, from beyond L2, which does not hold the rows of 1024 workgroups
 // (4096 x 12,288 in bf16 with a residual: 401 MB read, 201 needed).  Sums are in
 // f32: V * 8 products in a thread, then a tree over lanes and waves.  28,160 x 4096
-// in bf16: with a residual, and h, to 8 bits 127 us, 6.4 TB/s; gradients 147 us, 6.3
-// TB/s, and the sum of the workgroups' shares, 4.5 us.  4096 x 12,288: 92 us, 6.0
+// in bf16: with a residual, and h, to 8 bits 130 us, 6.2 TB/s; gradients 151 us, 6.1
+// TB/s, and the sum of the workgroups' shares, 5 us.  4096 x 12,288: 92 us, 6.0
 // TB/s of what is moved; gradients 84 us for dx, which reads dy and h twice, and 60
 // for dweight, which reads them once more.
 #include "vp_fp8_device.h"
